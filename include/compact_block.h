@@ -117,6 +117,10 @@ compact_status_t compact_fp8_product_status(compact_fp8_product_t* p);
 /* Selects the kernel: 0 = automatic, 1 = pairs of SMs, 2 = clusters that split K (the tests compare the two).  Returns
  * the previous value. */
 int compact_fp8_product_set_kernel(int which);
+/* Test hook that makes the choice of tiles observable, on the host alone: plan[0] the kernel of an automatic product (as above), and of
+ * the pairs' kernel plan[1] the columns of a tile, plan[2] the number of tiles, plan[3] the k-steps to a barrier, plan[4] the panels of
+ * column tiles that B is taken in. */
+compact_status_t compact_debug_fp8_product_plan(int64_t M, int64_t N, int64_t K, int32_t plan[5]);
 
 #ifdef __cplusplus
 }

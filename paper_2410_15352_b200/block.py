@@ -32,7 +32,7 @@ EXPORTS = [
     "compact_fp8_scale_groups", "compact_quantize_rows", "compact_quantize_blocks", "compact_rms_norm_fwd",
     "compact_rms_norm_bwd_workspace_bytes", "compact_rms_norm_bwd", "compact_rotary_create", "compact_rotary_destroy",
     "compact_rotary_apply", "compact_fp8_product_create", "compact_fp8_product_destroy", "compact_fp8_product_run",
-    "compact_fp8_product_status", "compact_fp8_product_set_kernel",
+    "compact_fp8_product_status", "compact_fp8_product_set_kernel", "compact_debug_fp8_product_plan",
 ]
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
@@ -72,6 +72,7 @@ def lib() -> C.CDLL:
     L.compact_fp8_product_run.argtypes = [vp, i64, i64, i64, C.c_int, vp, i64, vp, i64, C.c_int, vp, i64, vp, i64, C.c_int, vp, i64, vp]
     L.compact_fp8_product_status.argtypes = [vp]
     L.compact_fp8_product_set_kernel.argtypes = [C.c_int]
+    L.compact_debug_fp8_product_plan.argtypes = [i64, i64, i64, C.POINTER(i32)]
     _lib = L
     return L
 
@@ -184,6 +185,21 @@ class Fp8Product:
 def set_product_kernel(which: int) -> int:
     """0: automatic, 1: pairs of SMs, 2: clusters that split K.  Returns the previous choice."""
     return lib().compact_fp8_product_set_kernel(which)
+
+
+class ProductPlan(NamedTuple):
+    kernel: int           # of an automatic product: 1 or 2
+    width: int            # columns of a tile of the pairs' kernel
+    tiles: int
+    per_barrier: int      # k-steps
+    panels: int           # of column tiles
+
+
+def debug_product_plan(M: int, N: int, K: int) -> ProductPlan:
+    """What (M, K) by (N, K) is divided into (a test hook; nothing is launched)."""
+    plan = (C.c_int32 * 5)()
+    _check(lib().compact_debug_fp8_product_plan(M, N, K, plan), "compact_debug_fp8_product_plan")
+    return ProductPlan(*plan)
 
 
 # -- RMS norm ---------------------------------------------------------------------------------------

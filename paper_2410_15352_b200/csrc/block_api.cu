@@ -441,6 +441,18 @@ compact_status_t compact_fp8_product_status(compact_fp8_product_t* p) {
   return COMPACT_ERR_DEVICE_TIMEOUT;
 }
 
+compact_status_t compact_debug_fp8_product_plan(int64_t M, int64_t N, int64_t K, int32_t plan[5]) {
+  if (!plan || M < 1 || N < 1 || K < 1 || M > 0x7fffff00 || N > 0x7fffff00 || K > 0x7fffff00) return COMPACT_ERR_INVALID_ARG;
+  const PairPlan p = pair_plan((int)M, (int)N, (int)K);
+  if ((int64_t)p.tiles_m * p.tiles_n > 0x3fffffff) return COMPACT_ERR_SHAPE;
+  plan[0] = prefer_split((int)M, (int)N) ? 2 : 1;
+  plan[1] = p.bn;
+  plan[2] = p.tiles_m * p.tiles_n;
+  plan[3] = p.per_barrier;
+  plan[4] = (p.tiles_n + p.panel_cols - 1) / p.panel_cols;
+  return COMPACT_OK;
+}
+
 int compact_fp8_product_set_kernel(int which) {
   if (which < 0 || which > 2) return g_product_kernel.load();
   return g_product_kernel.exchange(which);

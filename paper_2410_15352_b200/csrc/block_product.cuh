@@ -751,27 +751,39 @@ inline int pair_bn(int tiles_m, int N) {
   return best;
 }
 
-inline compact_status_t product_pair(const ProductCall& c) {
-  static std::atomic<bool> attr[64];
-  if (!set_smem_once(product_pair_kernel, PP_SMEM_BYTES, attr)) return COMPACT_ERR_CUDA;
-  PairParams p;
-  memset(&p, 0, sizeof(p));
-  p.M = c.M; p.N = c.N;
-  p.ksteps = (c.K + PK - 1) / PK;
-  p.tiles_m = (c.M + 255) / 256;
-  p.bn = pair_bn(p.tiles_m, c.N);
-  p.tiles_n = (c.N + p.bn - 1) / p.bn;
+struct PairPlan {
+  int bn, tiles_m, tiles_n;
+  int per_barrier, panel_cols;      // as in PairParams
+};
+inline PairPlan pair_plan(int M, int N, int K) {
+  PairPlan p;
+  p.tiles_m = (M + 255) / 256;
+  p.bn = pair_bn(p.tiles_m, N);
+  p.tiles_n = (N + p.bn - 1) / p.bn;
   // Narrow tiles spend more time on barriers than on MMAs: two k-steps to each (256 x 4096 x 4096 9.2 us against 10.4).  Wide ones keep the
   // six stages of one, for the loads' sake (16384 x 4096 x 4096 214 us against 216).
   p.per_barrier = p.bn <= 128 ? 2 : 1;
   // B beyond 48 MB goes through the L2 in panels of column tiles (never narrower than a round of tiles is tall)
   p.panel_cols = p.tiles_n;
-  const long long b_bytes = (long long)c.K * c.N, most = 48ll << 20;
+  const long long b_bytes = (long long)K * N, most = 48ll << 20;
   if (b_bytes > most) {
     const int panels = (int)((b_bytes + most - 1) / most);
     p.panel_cols = (p.tiles_n + panels - 1) / panels;
     if (p.panel_cols < 8) p.panel_cols = p.tiles_n < 8 ? p.tiles_n : 8;
   }
+  return p;
+}
+
+inline compact_status_t product_pair(const ProductCall& c) {
+  static std::atomic<bool> attr[64];
+  if (!set_smem_once(product_pair_kernel, PP_SMEM_BYTES, attr)) return COMPACT_ERR_CUDA;
+  const PairPlan plan = pair_plan(c.M, c.N, c.K);
+  PairParams p;
+  memset(&p, 0, sizeof(p));
+  p.M = c.M; p.N = c.N;
+  p.ksteps = (c.K + PK - 1) / PK;
+  p.tiles_m = plan.tiles_m; p.tiles_n = plan.tiles_n; p.bn = plan.bn;
+  p.per_barrier = plan.per_barrier; p.panel_cols = plan.panel_cols;
   p.C = c.C; p.ldc = c.ldc; p.c_f32 = c.c_f32;
   p.idesc = mx_idesc(c.a_type, c.b_type, 256, p.bn);
   p.a.scales = (const uint32_t*)c.a_scales; p.a.lds = c.lds_a; p.a.rows = c.M;
