@@ -227,7 +227,6 @@ compact_status_t compact_rms_norm_bwd(int dtype, int64_t tokens, int32_t n, cons
   if (tokens < 0 || tokens > kMaxRows || n < 1) return COMPACT_ERR_INVALID_ARG;
   if (!dtype_ok(dtype)) return COMPACT_ERR_DTYPE;
   if (n > COMPACT_RMS_NORM_MAX_N) return COMPACT_ERR_SHAPE;
-  if (!dX && !dweight) return COMPACT_ERR_INVALID_ARG;
   if (!aligned4(dweight) || !aligned4(rstd)) return COMPACT_ERR_ALIGNMENT;
   cudaStream_t st = (cudaStream_t)stream;
   if (tokens == 0) {
@@ -237,7 +236,8 @@ compact_status_t compact_rms_norm_bwd(int dtype, int64_t tokens, int32_t n, cons
     if (cudaMemsetAsync(dweight, 0, (size_t)n * sizeof(float), st) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
     return COMPACT_OK;
   }
-  if (!dY || !H || !weight || !rstd) return COMPACT_ERR_INVALID_ARG;
+  // after the empty batch, whose dX has no memory
+  if (!dY || !H || !weight || !rstd || (!dX && !dweight)) return COMPACT_ERR_INVALID_ARG;
   const int64_t es = elem(dtype);
   if (!aligned16(dY) || !aligned16(H) || !aligned16(weight) || !pitch_ok(lddy, n, es) || !pitch_ok(ldh, n, es)) return COMPACT_ERR_ALIGNMENT;
   if (residual_grad && (!aligned16(residual_grad) || !pitch_ok(ldr, n, es))) return COMPACT_ERR_ALIGNMENT;
