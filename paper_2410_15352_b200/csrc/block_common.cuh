@@ -13,7 +13,9 @@ constexpr uint32_t SCALE_NAN = 255u;
 
 // Every kernel of this family is launched behind the one before it in its stream without waiting for its end (programmatic stream
 // serialization): it lets its own successor come up, prepares what needs no memory of others, and touches global memory
-// only when everything before it is done.  That hides a launch's start, 2 to 3 us, in a sequence of short calls.
+// only when everything before it is done.  That hides a launch's start, 2 to 3 us, in a sequence of short calls.  What it reads may
+// thus be written by its predecessor while it runs already: no pointer of these kernels is __restrict__, and nothing is read through
+// the read-only path (__ldg), whose loads may be moved ahead of the wait.
 __device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_predecessors() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -14,9 +14,8 @@ constexpr int QR_THREADS = QR_ROWS * 16;
 // independent, and it writes the word whole.  Neighbouring CTAs take neighbouring groups of the same eight rows.  What is read
 // once is marked so.  (16384 x 4096 bf16: 34.4 us, 5.9 TB/s; sixteen rows and 48 registers a thread 36.0.)
 template <typename T, int FP8>
-__global__ void __launch_bounds__(QR_THREADS, sizeof(T) == 2 ? 12 : 8) quantize_rows_kernel(const T* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
-                                                                   uint8_t* __restrict__ Q, int64_t ldq, uint32_t* __restrict__ scales,
-                                                                   int64_t lds, int groups) {
+__global__ void __launch_bounds__(QR_THREADS, sizeof(T) == 2 ? 12 : 8) quantize_rows_kernel(const T* X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* Q,
+                                                                                                       int64_t ldq, uint32_t* scales, int64_t lds, int groups) {
   let_successor_start();
   wait_for_predecessors();
   const int64_t tile = (int64_t)blockIdx.x / groups;
@@ -52,10 +51,10 @@ __global__ void __launch_bounds__(QR_THREADS, sizeof(T) == 2 ? 12 : 8) quantize_
 constexpr int QT_THREADS = 256;
 constexpr int QT_CTAS = 4;         // of bf16 blocks: 64 registers a thread
 template <typename T, int FP8>
-__global__ void __launch_bounds__(QT_THREADS, sizeof(T) == 2 ? QT_CTAS : 2) quantize_blocks_kernel(const T* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
-                                                                     uint8_t* __restrict__ Q, int64_t ldq, uint8_t* __restrict__ scales, int64_t lds,
-                                                                     uint8_t* __restrict__ QTr, int64_t ldqt, uint8_t* __restrict__ scales_t,
-                                                                     int64_t lds_t, int col_blocks) {
+__global__ void __launch_bounds__(QT_THREADS, sizeof(T) == 2 ? QT_CTAS : 2) quantize_blocks_kernel(const T* X, int64_t ldx, int64_t rows, int64_t cols,
+                                                                                                              uint8_t* Q, int64_t ldq, uint8_t* scales, int64_t lds,
+                                                                                                              uint8_t* QTr, int64_t ldqt, uint8_t* scales_t,
+                                                                                                              int64_t lds_t, int col_blocks) {
   __shared__ uint32_t tr[QB * 33];
   let_successor_start();
   wait_for_predecessors();
