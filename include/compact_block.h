@@ -63,7 +63,8 @@ compact_status_t compact_rms_norm_fwd(int dtype, int64_t tokens, int32_t n, floa
  *     dweight (fp32, n) = sum over tokens of dy * h * rstd
  * dx is the gradient of x and of the residual alike.  residual_grad (the gradient that reaches h past the norm), dX
  * or dweight may be NULL.  dX may be the same memory as dY or residual_grad.  accumulate != 0 adds to dweight.  The
- * order of the sum over tokens is fixed by (tokens, n): results are bitwise reproducible.
+ * order of the sum over tokens is fixed by (dtype, tokens, n) and by whether residual_grad is passed: results of the same call are
+ * bitwise reproducible, wherever its matrices lie and whichever outputs it has.
  * workspace: compact_rms_norm_bwd_workspace_bytes(dtype, tokens, n) bytes, not needed when dweight is NULL. */
 size_t compact_rms_norm_bwd_workspace_bytes(int dtype, int64_t tokens, int32_t n);
 compact_status_t compact_rms_norm_bwd(int dtype, int64_t tokens, int32_t n,

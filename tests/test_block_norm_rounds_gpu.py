@@ -110,3 +110,20 @@ def test_backward(tokens, n, dtype, extra):
         a, b = padded(dy, 32), None if dr is None else padded(dr, 48)
         got, none = norm.backward(a, h, w, rstd, residual_grad=b, dx=a if over_dy else b, need_dweight=False)
         assert none is None and torch.equal(got, dx)
+
+
+@pytest.mark.parametrize("extra", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tokens, n", [(10, 1000), (700, 1376), (3000, 600), (3000, 2048), (5001, 4096)])
+def test_the_order_of_the_weight_gradient(tokens, n, dtype, extra):
+    """The same bits wherever the matrices lie, with dx or without it, alone or after another."""
+    g, h, dr, w = inputs(tokens, n, dtype, extra)
+    dy = normal(g, (tokens, n), dtype)
+    norm = block.RMSNorm(n, eps=1e-5, dtype=dtype)
+    rstd = norm.forward(h, w).rstd
+    _, dw = norm.backward(padded(dy), h, w, rstd, residual_grad=dr)
+    _, alone = norm.backward(padded(dy, 64), padded(h, 32), w.clone(), rstd.clone(), residual_grad=None if dr is None else padded(dr, 16), need_dx=False)
+    assert torch.equal(dw, alone)
+    into = torch.zeros_like(dw)
+    norm.backward(padded(dy), h, w, rstd, residual_grad=dr, dweight=into, accumulate=True)
+    assert torch.equal(dw, into)
