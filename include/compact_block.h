@@ -80,7 +80,8 @@ compact_status_t compact_rms_norm_bwd(int dtype, int64_t tokens, int32_t n,
  *     COMPACT_ROTARY_LINEAR:   w_i / factor
  *     COMPACT_ROTARY_BASE:     the base is base * factor^(rot_dim / (rot_dim - 2))
  *     COMPACT_ROTARY_BY_PARTS: t = clamp((trained_length * w_i / 2 pi - low) / (high - low), 0, 1); w_i (t + (1 - t) / factor)
- * Angles are kept as 64-bit fractions of a turn, so they are as exact at position 10^6 as at 1. */
+ * Angles are kept as 64-bit fractions of a turn, so they are as exact at position 10^6 as at 1.  A factor that makes the base zero or
+ * infinite, or a w_i infinite, is refused. */
 typedef enum { COMPACT_ROTARY_NONE = 0, COMPACT_ROTARY_LINEAR = 1, COMPACT_ROTARY_BASE = 2, COMPACT_ROTARY_BY_PARTS = 3 } compact_rotary_scaling_t;
 typedef struct {
   int32_t head_dim, rot_dim;  /* rot_dim even, 2 <= rot_dim <= head_dim <= 1024, rot_dim <= 512 */

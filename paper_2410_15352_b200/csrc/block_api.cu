@@ -275,13 +275,12 @@ compact_status_t compact_rotary_create(const compact_rotary_config_t* cfg, compa
   if (cfg->scaling == COMPACT_ROTARY_BY_PARTS &&
       (!(cfg->high > cfg->low) || !(cfg->trained_length > 0.0) || !isfinite(cfg->low) || !isfinite(cfg->high) || !isfinite(cfg->trained_length)))
     return COMPACT_ERR_INVALID_ARG;
-  compact_rotary_t* r = new (std::nothrow) compact_rotary_t;
-  if (!r) return COMPACT_ERR_INVALID_ARG;
-  r->cfg = *cfg;
-  memset(&r->turns, 0, sizeof(r->turns));
+  RotaryTurns speeds;
+  memset(&speeds, 0, sizeof(speeds));
   const double two_pi = 6.283185307179586476925286766559, d = cfg->rot_dim;
   double base = cfg->base;
   if (cfg->scaling == COMPACT_ROTARY_BASE) base *= pow(cfg->factor, d / (d - 2.0));
+  if (!(base > 0.0) || !isfinite(base)) return COMPACT_ERR_INVALID_ARG;      // a factor that takes it out of range
   for (int i = 0; i < cfg->rot_dim / 2; ++i) {
     double w = pow(base, -2.0 * i / d);
     if (cfg->scaling == COMPACT_ROTARY_LINEAR) w /= cfg->factor;
@@ -290,10 +289,15 @@ compact_status_t compact_rotary_create(const compact_rotary_config_t* cfg, compa
       t = t < 0.0 ? 0.0 : (t > 1.0 ? 1.0 : t);
       w *= t + (1.0 - t) / cfg->factor;
     }
+    if (!isfinite(w)) return COMPACT_ERR_INVALID_ARG;
     // whole turns per position do not matter at whole positions
     const double turns = fmod(w / two_pi, 1.0) * 18446744073709551616.0;
-    r->turns.w[i] = turns >= 18446744073709551615.0 ? 0ull : (uint64_t)turns;
+    speeds.w[i] = turns >= 18446744073709551615.0 ? 0ull : (uint64_t)turns;
   }
+  compact_rotary_t* r = new (std::nothrow) compact_rotary_t;
+  if (!r) return COMPACT_ERR_INVALID_ARG;
+  r->cfg = *cfg;
+  r->turns = speeds;
   *out = r;
   return COMPACT_OK;
 }
