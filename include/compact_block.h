@@ -49,7 +49,7 @@ compact_status_t compact_quantize_blocks(int dtype, int64_t rows, int64_t cols, 
 
 /* RMS norm.  For each of `tokens` rows of n:
  *     h = x + residual            (rounded to the dtype; h = x when residual is NULL, and H must then be NULL)
- *     rstd = 1 / sqrt(mean(h^2) + eps)     (a row of zeros with eps = 0 gives NaN)
+ *     rstd = 1 / sqrt(mean(h^2) + eps)     (eps finite, not negative; a row of zeros with eps = 0 gives NaN)
  *     y = h * rstd * weight
  * Any of the outputs Y (dtype) and Q with scales (e4m3 or e5m2 of the unrounded y, a scale for each 128 columns) may be
  * NULL, and rstd (fp32, one per token, what the backward needs) too.  H may be the same memory as X or residual. */

@@ -217,7 +217,7 @@ class RMSNorm:
         self.code = _float_code(dtype, "RMSNorm")
         if not 1 <= n <= RMS_NORM_MAX_N:
             raise CompactError(ERR_SHAPE, "RMSNorm")
-        if not (eps >= 0.0 and math.isfinite(eps)):
+        if not (eps >= 0.0 and math.isfinite(C.c_float(eps).value)):      # as the kernel takes it
             raise CompactError(ERR_INVALID_ARG, "RMSNorm")
         self.n, self.eps, self.dtype = n, eps, dtype
 

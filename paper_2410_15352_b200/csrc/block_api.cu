@@ -191,7 +191,7 @@ compact_status_t compact_quantize_blocks(int dtype, int64_t rows, int64_t cols, 
 compact_status_t compact_rms_norm_fwd(int dtype, int64_t tokens, int32_t n, float eps, const void* X, int64_t ldx, const void* residual, int64_t ldr,
                                       const void* weight, void* H, int64_t ldh, void* Y, int64_t ldy, float* rstd, int fp8, void* Q, int64_t ldq,
                                       void* scales, int64_t lds, void* stream) {
-  if (tokens < 0 || tokens > kMaxRows || n < 1 || !(eps >= 0.f)) return COMPACT_ERR_INVALID_ARG;
+  if (tokens < 0 || tokens > kMaxRows || n < 1 || !(eps >= 0.f) || !isfinite(eps)) return COMPACT_ERR_INVALID_ARG;
   if (!dtype_ok(dtype) || (Q && fp8 != COMPACT_E4M3 && fp8 != COMPACT_E5M2)) return COMPACT_ERR_DTYPE;
   if (n > COMPACT_RMS_NORM_MAX_N) return COMPACT_ERR_SHAPE;
   if (tokens == 0) return COMPACT_OK;

@@ -25,3 +25,18 @@ def test_rotary_speeds_that_are_not_numbers_are_refused(kw):
                                 dict(scaling="by_parts", factor=1e-300), dict(base=1e300)])
 def test_rotary_speeds_at_the_ends_of_the_range(kw):
     block.Rotary(64, **kw)
+
+
+@pytest.mark.parametrize("eps", [float("inf"), float("nan"), -1.0, 1e39])
+def test_norm_eps_beyond_a_float_is_refused(eps):
+    """1e39 is finite as a double and infinite as the kernel's float, which would make every output zero."""
+    with pytest.raises(cb.CompactError) as e:
+        block.RMSNorm(64, eps=eps)
+    assert e.value.code == cb.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("tokens", [0, 4])
+def test_norm_infinite_eps_is_refused_by_the_library(tokens):
+    p = 0x1000      # an aligned address: no refused call looks behind it
+    call = block.lib().compact_rms_norm_fwd
+    assert call(cb.BF16, tokens, 64, float("inf"), p, 64, None, 0, p, None, 0, p, 64, None, 0, None, 0, None, 0, None) == cb.ERR_INVALID_ARG
