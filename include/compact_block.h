@@ -96,7 +96,8 @@ compact_status_t compact_rotary_destroy(compact_rotary_t* rot);
 /* Q [tokens x heads x head_dim] and K [tokens x kv_heads x head_dim] in one launch; K may be NULL with kv_heads = 0.
  * *_token and *_head are the strides, in elements, between tokens and between heads.  positions: one per token, int64
  * (pos_bits = 64) or int32 (32); NULL: token t is at first_position + t.  back != 0 applies the transpose (the gradient).
- * Outputs may be the inputs themselves; they must not overlap them in another way. */
+ * Outputs may be the inputs themselves; they must not overlap them in another way, nor themselves: an output's strides are at least
+ * head_dim long (of a single token or head they are not used).  Those of an input are free. */
 compact_status_t compact_rotary_apply(const compact_rotary_t* rot, int dtype, int64_t tokens, int32_t heads, int32_t kv_heads,
                                       const void* Q, int64_t q_token, int64_t q_head, const void* K, int64_t k_token, int64_t k_head,
                                       const void* positions, int pos_bits, int64_t first_position, int back,

@@ -317,6 +317,10 @@ compact_status_t compact_rotary_apply(const compact_rotary_t* rot, int dtype, in
   if (positions && pos_bits != 64 && pos_bits != 32) return COMPACT_ERR_DTYPE;
   if (tokens == 0) return COMPACT_OK;
   if (!Q || !Qout || (kv_heads > 0 && (!K || !Kout))) return COMPACT_ERR_INVALID_ARG;
+  // heads written closer together than they are long, or all to one place, would run into each other
+  const int64_t d = rot->cfg.head_dim;
+  const auto apart = [d](int64_t stride, int64_t count) { return count <= 1 || stride >= d || stride <= -d; };
+  if (!apart(qo_token, tokens) || !apart(qo_head, heads) || (kv_heads && (!apart(ko_token, tokens) || !apart(ko_head, kv_heads)))) return COMPACT_ERR_INVALID_ARG;
   const int es = (int)elem(dtype), V16 = 16 / es;
   const uintptr_t at = reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(Qout) |
                        (kv_heads ? reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(Kout) : 0);
