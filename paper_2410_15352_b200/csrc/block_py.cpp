@@ -121,6 +121,17 @@ at::Tensor given_or(PyObject* o, Make make) {
   return o == Py_None ? make() : tensor(o);
 }
 
+// Tensors that the caller brought and the call has written: autograd must not take what it saved of them for what they are now.
+template <class... P>
+void written(P*... o) {
+  const auto one = [](PyObject* p) {
+    if (p == Py_None) return;
+    const at::Tensor& t = tensor(p);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  };
+  (one(o), ...);
+}
+
 // Without the interpreter's lock: a launch may wait for room in the stream.
 struct Unlocked {
   PyThreadState* state = PyEval_SaveThread();
@@ -183,6 +194,7 @@ PyObject* quantize_rows_impl(PyObject* const* a) {
   run(c.where, [&] {
     return api.quantize_rows(code, rows, cols, x.data_ptr(), ldx, (int)fp8, q.data_ptr(), ldq, s.data_ptr(), lds, c.stream());
   });
+  written(a[2], a[3]);
   return tuple(q, s);
 }
 ENTRY(quantize_rows, 4)
@@ -212,6 +224,7 @@ PyObject* quantize_blocks_impl(PyObject* const* a) {
     return api.quantize_blocks(code, rows, cols, x.data_ptr(), ldx, (int)fp8, q.data_ptr(), ldq, s.data_ptr(), lds, both ? qt.data_ptr() : nullptr, ldqt,
                                both ? st.data_ptr() : nullptr, ldst, c.stream());
   });
+  written(a[2], a[3], a[5], a[6]);
   return tuple(q, s, qt, st);
 }
 ENTRY(quantize_blocks, 7)
@@ -261,6 +274,7 @@ PyObject* rms_norm_fwd_impl(PyObject* const* a) {
     return api.rms_norm_fwd((int)code, tokens, (int32_t)n, (float)eps, x.data_ptr(), ldx, res, ldr, w, hp, ldh, yp, ldy, (float*)rstd.data_ptr(), fp8, qp,
                             ldq, sp, lds, c.stream());
   });
+  written(a[6], a[8], a[11], a[12]);
   return tuple(h, y, rstd, q, s);
 }
 ENTRY(rms_norm_fwd, 13)
@@ -305,6 +319,7 @@ PyObject* rms_norm_bwd_impl(PyObject* const* a) {
     return api.rms_norm_bwd((int)code, tokens, (int32_t)n, dy.data_ptr(), lddy, h.data_ptr(), ldh, w, (const float*)rstd, res, ldr, dxp, lddx, dwp, accumulate,
                             wsp, ws_bytes, c.stream());
   });
+  written(a[8], a[10]);
   return tuple(dx, dw);
 }
 ENTRY(rms_norm_bwd, 12)
@@ -358,6 +373,7 @@ PyObject* rotary_apply_impl(PyObject* const* a) {
                             ks.head, pos, bits, first, back, qo.data_ptr(), qos.token, qos.head, kv ? ko.data_ptr() : nullptr, kos.token, kos.head,
                             c.stream());
   });
+  written(a[7], a[8]);
   return tuple(qo, ko);
 }
 ENTRY(rotary_apply, 9)
@@ -377,6 +393,7 @@ PyObject* fp8_product_impl(PyObject* const* a) {
     return api.fp8_product_run(handle, M, N, K, at_, A.data_ptr(), lda, sa.data_ptr(), la, bt, B.data_ptr(), ldb, sb.data_ptr(), lb, ct, out.data_ptr(), ldc,
                                c.stream());
   });
+  written(a[5]);
   return wrap(out);
 }
 ENTRY(fp8_product, 7)
