@@ -120,6 +120,11 @@ compact_status_t compact_fp8_product_status(compact_fp8_product_t* p);
 /* Selects the kernel: 0 = automatic, 1 = pairs of SMs, 2 = clusters that split K (the tests compare the two).  Returns
  * the previous value. */
 int compact_fp8_product_set_kernel(int which);
+/* Test hook for the bounded waits: the handle's next product loads only the first `k_steps` of the 128-column steps of each tile's K (rounded
+ * up to the even number that share a barrier), and its waits give up after a few thousand polls.  With fewer steps than K has, the
+ * kernel gives up as it would after a lost copy: it returns, C is not valid, compact_fp8_product_status reports
+ * COMPACT_ERR_DEVICE_TIMEOUT once, and the context stays usable.  k_steps < 0 takes the request back. */
+compact_status_t compact_debug_fp8_product_withhold(compact_fp8_product_t* p, int32_t k_steps);
 /* Test hook that makes the choice of tiles observable, on the host alone: plan[0] the kernel of an automatic product (as above), and of
  * the pairs' kernel plan[1] the columns of a tile, plan[2] the number of tiles, plan[3] the k-steps to a barrier, plan[4] the panels of
  * column tiles that B is taken in. */

@@ -32,7 +32,8 @@ EXPORTS = [
     "compact_fp8_scale_groups", "compact_quantize_rows", "compact_quantize_blocks", "compact_rms_norm_fwd",
     "compact_rms_norm_bwd_workspace_bytes", "compact_rms_norm_bwd", "compact_rotary_create", "compact_rotary_destroy",
     "compact_rotary_apply", "compact_fp8_product_create", "compact_fp8_product_destroy", "compact_fp8_product_run",
-    "compact_fp8_product_status", "compact_fp8_product_set_kernel", "compact_debug_fp8_product_plan",
+    "compact_fp8_product_status", "compact_fp8_product_set_kernel", "compact_debug_fp8_product_withhold",
+    "compact_debug_fp8_product_plan",
 ]
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
@@ -72,6 +73,7 @@ def lib() -> C.CDLL:
     L.compact_fp8_product_run.argtypes = [vp, i64, i64, i64, C.c_int, vp, i64, vp, i64, C.c_int, vp, i64, vp, i64, C.c_int, vp, i64, vp]
     L.compact_fp8_product_status.argtypes = [vp]
     L.compact_fp8_product_set_kernel.argtypes = [C.c_int]
+    L.compact_debug_fp8_product_withhold.argtypes = [vp, i32]
     L.compact_debug_fp8_product_plan.argtypes = [i64, i64, i64, C.POINTER(i32)]
     _lib = L
     return L
@@ -180,6 +182,10 @@ class Fp8Product:
     def status(self) -> int:
         """Reads and clears the status word (synchronises the device)."""
         return int(lib().compact_fp8_product_status(self._h))
+
+    def debug_withhold(self, k_steps: int) -> None:
+        """The next product loads only that many k-steps of each tile and gives up waiting for the rest after a few thousand polls (a test hook)."""
+        _check(lib().compact_debug_fp8_product_withhold(self._h, k_steps), "compact_debug_fp8_product_withhold")
 
 
 def set_product_kernel(which: int) -> int:

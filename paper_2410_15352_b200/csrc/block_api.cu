@@ -28,6 +28,7 @@ struct compact_rotary {
 struct compact_fp8_product {
   int slot;
   int touched_device;     // -1: nothing launched yet
+  int next_loaded;        // k-steps that the next product loads; -1: all
 };
 
 namespace {
@@ -374,6 +375,7 @@ compact_status_t compact_fp8_product_create(compact_fp8_product_t** out) {
   compact_fp8_product_t* p = new (std::nothrow) compact_fp8_product_t;
   if (!p) return COMPACT_ERR_INVALID_ARG;
   p->touched_device = -1;
+  p->next_loaded = -1;
   {
     std::lock_guard<std::mutex> lock(g_slot_mutex);
     p->slot = -1;
@@ -422,12 +424,16 @@ compact_status_t compact_fp8_product_run(compact_fp8_product_t* p, int64_t M, in
   c.a_type = a_type; c.b_type = b_type; c.A = A; c.B = B; c.a_scales = a_scales; c.b_scales = b_scales;
   c.lda = lda; c.ldb = ldb; c.lds_a = lds_a; c.lds_b = lds_b;
   c.c_f32 = c_dtype == COMPACT_F32; c.C = C; c.ldc = ldc;
-  c.status = product_status(dev, p->slot);
-  if (!c.status) return COMPACT_ERR_CUDA;
+  c.waits.status = product_status(dev, p->slot);
+  if (!c.waits.status) return COMPACT_ERR_CUDA;
+  const bool short_waits = p->next_loaded >= 0;
+  c.waits.limit = short_waits ? 4096u : tc::WAIT_LIMIT;
+  c.waits.loaded = short_waits ? p->next_loaded : c.K;      // no fewer than the k-steps
+  p->next_loaded = -1;
   c.stream = (cudaStream_t)stream;
   if (p->touched_device != dev) {
     // the slot may have belonged to a handle that was destroyed without its status having been read
-    if (cudaMemsetAsync(c.status, 0, sizeof(unsigned int), c.stream) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
+    if (cudaMemsetAsync(c.waits.status, 0, sizeof(unsigned int), c.stream) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
     p->touched_device = dev;
   }
   const int which = g_product_kernel.load();
@@ -447,6 +453,12 @@ compact_status_t compact_fp8_product_status(compact_fp8_product_t* p) {
   v = 0;
   cudaMemcpy(w, &v, 4, cudaMemcpyHostToDevice);
   return COMPACT_ERR_DEVICE_TIMEOUT;
+}
+
+compact_status_t compact_debug_fp8_product_withhold(compact_fp8_product_t* p, int32_t k_steps) {
+  if (!p) return COMPACT_ERR_INVALID_ARG;
+  p->next_loaded = k_steps < 0 ? -1 : k_steps;
+  return COMPACT_OK;
 }
 
 compact_status_t compact_debug_fp8_product_plan(int64_t M, int64_t N, int64_t K, int32_t plan[5]) {

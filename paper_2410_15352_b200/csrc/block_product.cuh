@@ -38,6 +38,17 @@ struct ProductOperand {
   int rows;
 };
 
+// What the waits of a launch are bounded by and report to.  `loaded`: k-steps of a tile that are loaded, all of them but in the test that
+// makes the waits run out.
+struct ProductWaits {
+  unsigned int* status;
+  uint32_t limit;            // polls
+  int loaded;
+};
+__device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, const ProductWaits& w) {
+  return mbar_wait(bar, parity, abort_flag, w.status, w.limit);
+}
+
 // ---- pairs of SMs -----------------------------------------------------------------------------------
 constexpr int PP_NS = 6;
 constexpr int PP_STAGE_BYTES = 2 * P_TILE_BYTES;     // [A: 128 rows | B: up to 128 rows]
@@ -69,7 +80,7 @@ struct alignas(64) PairParams {
   int c_f32;
   int per_barrier;                        // k-steps (stages) that share a barrier
   uint32_t idesc;                         // types and shape of the instruction, without the byte numbers of the scales
-  unsigned int* status;
+  ProductWaits waits;
 };
 
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&v)[4]) {
@@ -297,7 +308,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) product_pair_kernel(const __gri
       m0 += (int)crank * 128;
       n0 += (int)crank * half_bn;
       for (int ks = 0; ks < prm.ksteps; ks += prm.per_barrier) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, prm.status)))) break;
+        if (!(ok = ks < prm.waits.loaded)) break;
+        if (!(ok = __all_sync(0xffffffffu, bounded_wait(empty_bar(s), ph ^ 1u, abort_flag, prm.waits)))) break;
         if (elect_one()) {
           const int count = min(prm.per_barrier, prm.ksteps - ks);
           if (leader) mbar_arrive_expect_tx(full_bar(s), bytes * (uint32_t)count);
@@ -320,18 +332,18 @@ __global__ void __launch_bounds__(PP_THREADS, 1) product_pair_kernel(const __gri
       uint32_t ph = 0, tph = 0, slot_phase = 0, shared_phase = 0;
       const uint32_t ring_lo = ((smem_base >> 4) & 0x3FFFu) | (1u << 16);
       for (int tile = pair_id; tile < total && ok; tile += npairs) {
-        if (!(ok = mbar_wait(tempty_bar(slot), slot_phase ^ 1u, abort_flag, prm.status))) break;
+        if (!(ok = bounded_wait(tempty_bar(slot), slot_phase ^ 1u, abort_flag, prm.waits))) break;
         if (prm.bn > PP_SLOT_COLS && tile != pair_id) {
-          if (!(ok = mbar_wait(shared_bar, shared_phase, abort_flag, prm.status))) break;
+          if (!(ok = bounded_wait(shared_bar, shared_phase, abort_flag, prm.waits))) break;
           shared_phase ^= 1u;
         }
         tc_fence_after();
         const uint32_t d = tmem_base + (uint32_t)(slot * PP_SLOT_COLS);
         for (int ks = 0; ks < prm.ksteps; ks += prm.per_barrier) {
           if ((ks & 3) == 0) {
-            if (!(ok = mbar_wait(sfull_bar(t), tph, abort_flag, prm.status))) break;
+            if (!(ok = bounded_wait(sfull_bar(t), tph, abort_flag, prm.waits))) break;
           }
-          if (!(ok = mbar_wait(full_bar(s), ph, abort_flag, prm.status))) break;
+          if (!(ok = bounded_wait(full_bar(s), ph, abort_flag, prm.waits))) break;
           tc_fence_after();
           const uint32_t sa = tmem_base + PP_SF_COL + 16u * t, sb = sa + 4;
           const int end = min(ks + prm.per_barrier, prm.ksteps);
@@ -370,7 +382,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) product_pair_kernel(const __gri
     for (int tile = pair_id; tile < total && ok; tile += npairs) {
       int m0, n0;
       pair_tile(prm, tile, m0, n0);
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(slot), slot_phase, abort_flag, prm.status)))) break;
+      if (!(ok = __all_sync(0xffffffffu, bounded_wait(tfull_bar(slot), slot_phase, abort_flag, prm.waits)))) break;
       tc_fence_after();
       const int row0 = m0 + (int)crank * 128 + q * 32;
       const uint32_t tcol = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(slot * PP_SLOT_COLS);
@@ -439,7 +451,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) product_pair_kernel(const __gri
       cp_async_wait<SF_AHEAD - 1>();
       named_barrier(1, 128);                                // all four quarters of this group have landed, and the previous one is read
       fetch_next();
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(sempty_bar(t), tph ^ 1u, abort_flag, prm.status));
+      if (ok) ok = __all_sync(0xffffffffu, bounded_wait(sempty_bar(t), tph ^ 1u, abort_flag, prm.waits));
       if (ok) {
         tc_fence_after();
         const uint32_t at = tmem_base + quarter + PP_SF_COL + 16u * t, src = buffer(rb);
@@ -490,7 +502,7 @@ struct alignas(64) SplitParams {
   int64_t ldc;
   int M, N, bt, splits, ksteps, stages, c_f32;
   uint32_t idesc;
-  unsigned int* status;
+  ProductWaits waits;
 };
 
 // k-steps of each CTA of a cluster: an even number
@@ -553,7 +565,8 @@ __global__ void __launch_bounds__(PS_THREADS, 1) product_split_kernel(const __gr
     int s = 0;
     uint32_t ph = 0;
     for (int ks = k_begin; ks < k_end; ks += 2) {
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, prm.status)))) break;
+      if (!(ok = ks < prm.waits.loaded)) break;
+      if (!(ok = __all_sync(0xffffffffu, bounded_wait(empty_bar(s), ph ^ 1u, abort_flag, prm.waits)))) break;
       if (elect_one()) {
         mbar_arrive_expect_tx(full_bar(s), stage_bytes);
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
@@ -573,9 +586,9 @@ __global__ void __launch_bounds__(PS_THREADS, 1) product_split_kernel(const __gr
       uint32_t ph = 0, tph = 0;
       for (int ks = k_begin; ks < k_end; ks += 2) {
         if (ks == k_begin || (ks & 3) == 0) {
-          if (!(ok = mbar_wait(sfull_bar(t), tph, abort_flag, prm.status))) break;
+          if (!(ok = bounded_wait(sfull_bar(t), tph, abort_flag, prm.waits))) break;
         }
-        if (!(ok = mbar_wait(full_bar(s), ph, abort_flag, prm.status))) break;
+        if (!(ok = bounded_wait(full_bar(s), ph, abort_flag, prm.waits))) break;
         tc_fence_after();
         const uint32_t sa = tmem_base + PS_SF_COL + 8u * t, sb = sa + 4;
 #pragma unroll
@@ -622,7 +635,7 @@ __global__ void __launch_bounds__(PS_THREADS, 1) product_split_kernel(const __gr
       cp_async_wait<SF_AHEAD - 1>();
       named_barrier(1, 128);
       fetch_next();
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(sempty_bar(t), tph ^ 1u, abort_flag, prm.status));
+      if (ok) ok = __all_sync(0xffffffffu, bounded_wait(sempty_bar(t), tph ^ 1u, abort_flag, prm.waits));
       if (ok) {
         tc_fence_after();
         const uint32_t at = tmem_base + quarter + PS_SF_COL + 8u * t, src = sbuf + (uint32_t)rb * 1024u;
@@ -637,7 +650,7 @@ __global__ void __launch_bounds__(PS_THREADS, 1) product_split_kernel(const __gr
       if (++rb == SF_BUFS) rb = 0;
     }
     cp_async_wait<0>();
-    if (ok && k_begin < k_end) ok = __all_sync(0xffffffffu, mbar_wait(tfull, 0u, abort_flag, prm.status));
+    if (ok && k_begin < k_end) ok = __all_sync(0xffffffffu, bounded_wait(tfull, 0u, abort_flag, prm.waits));
     tc_fence_after();
   }
 
@@ -734,7 +747,7 @@ struct ProductCall {
   int c_f32;
   void* C;
   int64_t ldc;
-  unsigned int* status;
+  ProductWaits waits;
   cudaStream_t stream;
 };
 
@@ -788,7 +801,7 @@ inline compact_status_t product_pair(const ProductCall& c) {
   p.idesc = mx_idesc(c.a_type, c.b_type, 256, p.bn);
   p.a.scales = (const uint32_t*)c.a_scales; p.a.lds = c.lds_a; p.a.rows = c.M;
   p.b.scales = (const uint32_t*)c.b_scales; p.b.lds = c.lds_b; p.b.rows = c.N;
-  p.status = c.status;
+  p.waits = c.waits;
   if (!make_map_8bit(&p.tmA, c.A, c.K, c.M, c.lda, 128)) return COMPACT_ERR_CUDA;
   if (!make_map_8bit(&p.tmB, c.B, c.K, c.N, c.ldb, p.bn / 2)) return COMPACT_ERR_CUDA;
   const long long total = (long long)p.tiles_m * p.tiles_n;
@@ -850,7 +863,7 @@ inline compact_status_t product_split(const ProductCall& c) {
   p.idesc = mx_idesc(c.b_type, c.a_type, 128, p.bt);
   p.w.scales = (const uint32_t*)c.b_scales; p.w.lds = c.lds_b; p.w.rows = c.N;
   p.x.scales = (const uint32_t*)c.a_scales; p.x.lds = c.lds_a; p.x.rows = c.M;
-  p.status = c.status;
+  p.waits = c.waits;
   if (!make_map_8bit(&p.tmW, c.B, c.K, c.N, c.ldb, 128)) return COMPACT_ERR_CUDA;
   if (!make_map_8bit(&p.tmX, c.A, c.K, c.M, c.lda, p.bt)) return COMPACT_ERR_CUDA;
   return launch(product_split_kernel, dim3(tiles_n * splits, tiles_m), PS_THREADS, PS_SMEM_BYTES, splits, c.stream, p);

@@ -50,9 +50,10 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait: gives up after about a second, records it, and lets the CTA drain.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned int* status,
-                                          uint32_t limit = 8000000u) {
+// Bounded wait: gives up after about a second, records it by `expired`, and lets the CTA drain.
+constexpr uint32_t WAIT_LIMIT = 8000000u;      // polls
+template <class Expired>
+__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, volatile int* abort_flag, Expired expired, uint32_t limit) {
   if (mbar_try_wait(bar, parity)) return true;
   for (uint32_t it = 0; it < limit; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -62,8 +63,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
   }
   *abort_flag = 1;
-  atomicOr(status, STATUS_TIMEOUT);
+  expired();
   return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned int* status,
+                                          uint32_t limit = WAIT_LIMIT) {
+  return mbar_wait_or(bar, parity, abort_flag, [status] { atomicOr(status, STATUS_TIMEOUT); }, limit);
 }
 
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
