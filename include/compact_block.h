@@ -115,7 +115,9 @@ compact_status_t compact_fp8_product_run(compact_fp8_product_t* p, int64_t M, in
                                          int a_type, const void* A, int64_t lda, const void* a_scales, int64_t lds_a,
                                          int b_type, const void* B, int64_t ldb, const void* b_scales, int64_t lds_b,
                                          int c_dtype, void* C, int64_t ldc, void* stream);
-/* Reads and clears the status word (synchronises the device), as compact_layer_status does for a layer. */
+/* COMPACT_ERR_DEVICE_TIMEOUT if one of the handle's kernels has given up on a wait since the last call (its C is then not valid), on whichever
+ * device and stream it ran, replayed from a graph or not; COMPACT_OK otherwise.  Synchronises the devices that the handle has launched
+ * on.  After the handle is destroyed there is nobody to tell: one whose products matter outlives them. */
 compact_status_t compact_fp8_product_status(compact_fp8_product_t* p);
 /* Selects the kernel: 0 = automatic, 1 = pairs of SMs, 2 = clusters that split K (the tests compare the two).  Returns
  * the previous value. */

@@ -7,8 +7,9 @@ over by a small C++ module (csrc/block_py.cpp); if it or the library is missing,
 
     x8 = RMSNorm(n).forward(x, gamma, residual=r, want_fp8=True).q     # what the next product reads
     w8, w8t = quantize_blocks(W)                                       # a layer's weight (n x m) and its transpose, once per update
-    y = Fp8Product()(x8, w8t)                                          # Y = X W
-    dx = Fp8Product()(quantize_rows(dy), w8)                           # dX = dY W^T
+    product = Fp8Product()                                             # kept: it is asked for its status now and then
+    y = product(x8, w8t)                                               # Y = X W
+    dx = product(quantize_rows(dy), w8)                                # dX = dY W^T
     q, k = Rotary(128).forward(q, k, positions)
 """
 from __future__ import annotations
@@ -180,7 +181,8 @@ class Fp8Product:
         return self._run(self._h.value, a.data, a.scales, b.data, b.scales, out, _float_code(dtype, "compact_fp8_product_run"))
 
     def status(self) -> int:
-        """Reads and clears the status word (synchronises the device)."""
+        """ERR_DEVICE_TIMEOUT if a kernel of this handle has given up on a wait since the last call, on any device or in a graph; OK
+        otherwise.  Synchronises the devices that the handle has launched on."""
         return int(lib().compact_fp8_product_status(self._h))
 
     def debug_withhold(self, k_steps: int) -> None:

@@ -27,7 +27,8 @@ struct compact_rotary {
 
 struct compact_fp8_product {
   int slot;
-  int touched_device;     // -1: nothing launched yet
+  uint32_t tag;           // its mark in the slot's word
+  uint64_t devices;       // those it has launched on, a bit each
   int next_loaded;        // k-steps that the next product loads; -1: all
 };
 
@@ -64,11 +65,15 @@ compact_status_t check_device(int* device) {
 
 
 // ---- status words of the products' bounded waits ---------------------------------------------------
+// A word per slot and device, zero at load.  A wait that runs out writes its handle's tag there (the largest stays), and a handle asks whether
+// the word holds its own.  So no launch has to clear what a slot's earlier handle left, which would also clear, captured into a graph and
+// replayed or coming back from another device, what its own kernels reported; and a kernel that outlives its handle reports to nobody else.
 constexpr int kProductSlots = 1024;
 __device__ unsigned int g_product_status[kProductSlots];
 std::mutex g_slot_mutex;
 std::vector<int> g_free_slots;
 int g_slots_out = 0;
+uint32_t g_slot_tags[kProductSlots];      // of the slots' last handles
 std::atomic<int> g_product_kernel{0};
 
 unsigned int* product_status(int dev, int slot) {
@@ -374,7 +379,7 @@ compact_status_t compact_fp8_product_create(compact_fp8_product_t** out) {
   *out = nullptr;
   compact_fp8_product_t* p = new (std::nothrow) compact_fp8_product_t;
   if (!p) return COMPACT_ERR_INVALID_ARG;
-  p->touched_device = -1;
+  p->devices = 0;
   p->next_loaded = -1;
   {
     std::lock_guard<std::mutex> lock(g_slot_mutex);
@@ -390,6 +395,7 @@ compact_status_t compact_fp8_product_create(compact_fp8_product_t** out) {
       } catch (...) {
       }
     }
+    if (p->slot >= 0) p->tag = ++g_slot_tags[p->slot];
   }
   if (p->slot < 0) { delete p; return COMPACT_ERR_TOO_MANY_LAYERS; }
   *out = p;
@@ -430,12 +436,9 @@ compact_status_t compact_fp8_product_run(compact_fp8_product_t* p, int64_t M, in
   c.waits.limit = short_waits ? 4096u : tc::WAIT_LIMIT;
   c.waits.loaded = short_waits ? p->next_loaded : c.K;      // no fewer than the k-steps
   p->next_loaded = -1;
+  c.waits.tag = p->tag;
   c.stream = (cudaStream_t)stream;
-  if (p->touched_device != dev) {
-    // the slot may have belonged to a handle that was destroyed without its status having been read
-    if (cudaMemsetAsync(c.waits.status, 0, sizeof(unsigned int), c.stream) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
-    p->touched_device = dev;
-  }
+  p->devices |= (uint64_t)1 << dev;
   const int which = g_product_kernel.load();
   const bool split = which == 2 || (which == 0 && prefer_split(c.M, c.N));
   return split ? product_split(c) : product_pair(c);
@@ -443,16 +446,27 @@ compact_status_t compact_fp8_product_run(compact_fp8_product_t* p, int64_t M, in
 
 compact_status_t compact_fp8_product_status(compact_fp8_product_t* p) {
   if (!p) return COMPACT_ERR_INVALID_ARG;
-  if (p->touched_device < 0) return COMPACT_OK;
-  unsigned int* w = product_status(p->touched_device, p->slot);
-  if (!w) return COMPACT_ERR_CUDA;
-  unsigned int v = 0;
-  if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
-  if (cudaMemcpy(&v, w, 4, cudaMemcpyDeviceToHost) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
-  if (!v) return COMPACT_OK;
-  v = 0;
-  cudaMemcpy(w, &v, 4, cudaMemcpyHostToDevice);
-  return COMPACT_ERR_DEVICE_TIMEOUT;
+  if (!p->devices) return COMPACT_OK;
+  int current = 0;
+  if (cudaGetDevice(&current) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
+  compact_status_t result = COMPACT_OK;
+  for (int dev = 0; dev < kMaxDevices; ++dev) {
+    if (!(p->devices >> dev & 1)) continue;
+    unsigned int v = 0;
+    unsigned int* w = nullptr;
+    if (cudaSetDevice(dev) != cudaSuccess || !(w = product_status(dev, p->slot)) || cudaDeviceSynchronize() != cudaSuccess ||
+        cudaMemcpy(&v, w, sizeof(v), cudaMemcpyDeviceToHost) != cudaSuccess) {
+      cudaGetLastError();
+      result = COMPACT_ERR_CUDA;
+      continue;
+    }
+    if (v != p->tag) continue;
+    v = 0;
+    if (cudaMemcpy(w, &v, sizeof(v), cudaMemcpyHostToDevice) != cudaSuccess) { cudaGetLastError(); result = COMPACT_ERR_CUDA; }
+    if (result == COMPACT_OK) result = COMPACT_ERR_DEVICE_TIMEOUT;
+  }
+  if (cudaSetDevice(current) != cudaSuccess) { cudaGetLastError(); return COMPACT_ERR_CUDA; }
+  return result;
 }
 
 compact_status_t compact_debug_fp8_product_withhold(compact_fp8_product_t* p, int32_t k_steps) {

@@ -42,11 +42,12 @@ struct ProductOperand {
 // makes the waits run out.
 struct ProductWaits {
   unsigned int* status;
+  uint32_t tag;              // the handle's mark: of two handles that have had a word in turn, the later has the larger one
   uint32_t limit;            // polls
   int loaded;
 };
 __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, const ProductWaits& w) {
-  return mbar_wait(bar, parity, abort_flag, w.status, w.limit);
+  return mbar_wait_or(bar, parity, abort_flag, [&w] { atomicMax(w.status, w.tag); }, w.limit);
 }
 
 // ---- pairs of SMs -----------------------------------------------------------------------------------

@@ -65,3 +65,59 @@ def test_all_steps_loaded_is_an_ordinary_product():
     p.debug_withhold(6)
     assert torch.equal(p(a, b), want) and p.status() == cb.OK
     assert want.dtype == BF
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [1, 2])
+def test_a_replayed_graph_forgets_nothing(which):
+    """A handle whose first product was captured: replays must not clear what an earlier product, or an earlier replay, reported."""
+    build_library()
+    a, b = operands(7, 200, 256, 700)
+    block.set_product_kernel(which)
+    try:
+        want = block.Fp8Product()(a, b)
+        p, out = block.Fp8Product(), torch.empty_like(want)
+        good, bad = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(good):
+            p(a, b, out=out)
+        p.debug_withhold(2)
+        with torch.cuda.graph(bad):
+            p(a, b, out=out)
+        good.replay()
+        assert p.status() == cb.OK and torch.equal(out, want)
+        bad.replay()
+        good.replay()
+        good.replay()
+        assert p.status() == cb.ERR_DEVICE_TIMEOUT and torch.equal(out, want)
+        assert p.status() == cb.OK
+        p.debug_withhold(0)
+        p(a, b, out=out)
+        good.replay()
+        assert p.status() == cb.ERR_DEVICE_TIMEOUT and torch.equal(out, want)
+    finally:
+        block.set_product_kernel(0)
+
+
+@pytest.mark.gpu
+def test_a_slot_passes_from_handle_to_handle():
+    """What an earlier handle of the slot left is not taken for the later one's, and does not hide it."""
+    build_library()
+    a, b = operands(8, 200, 256, 700)
+    first = block.Fp8Product()
+    first.debug_withhold(0)
+    first(a, b)
+    del first                                                          # unread, and perhaps still running
+    second = block.Fp8Product()                                        # in its slot
+    second(a, b)
+    assert second.status() == cb.OK
+    second.debug_withhold(0)
+    second(a, b)
+    assert second.status() == cb.ERR_DEVICE_TIMEOUT and second.status() == cb.OK
+    second.debug_withhold(0)
+    second(a, b)
+    del second
+    assert block.Fp8Product().status() == cb.OK                        # nothing launched
+    third = block.Fp8Product()
+    third(a, b)
+    assert third.status() == cb.OK
