@@ -23,7 +23,7 @@ import torch
 
 from . import binding as cb
 from .binding import BF16, ERR_DTYPE, ERR_INVALID_ARG, ERR_SHAPE, F32, CompactError
-from .build import LIB_PATH
+from .build import LIB_PATH, MODULE_PATH, module_fits, module_tag
 
 E4M3, E5M2 = 0, 1
 ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BY_PARTS = range(4)
@@ -85,6 +85,8 @@ def _module():
     global _mod
     if _mod is None:
         lib()
+        if not module_fits():
+            raise ImportError(f"{MODULE_PATH} is missing, or built for another Python or torch than {module_tag()}: build.build_module() makes it")
         from . import _block_py
 
         _block_py.open_library(LIB_PATH, CompactError)

@@ -422,4 +422,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block_py", nullptr, -1, methods, 
 
 }  // namespace
 
+// The Python and torch that the module was built for, found in its file by build.module_fits before it is loaded
+extern "C" __attribute__((visibility("default"), used)) const char compact_block_py_tag[] = "built for [" BUILT_FOR "]";
+
 PyMODINIT_FUNC PyInit__block_py() { return PyModule_Create(&module); }
