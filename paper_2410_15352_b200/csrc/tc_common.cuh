@@ -271,8 +271,11 @@ inline bool encode_cached(CUtensorMap* map, CUtensorMapDataType type, uint32_t r
   if (fn(map, type, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
-  if (cache.size() >= 8192) cache.clear();
-  cache.emplace(key, *map);
+  try {
+    if (cache.size() >= 8192) cache.clear();
+    cache.emplace(key, *map);
+  } catch (...) {      // without memory to keep it, it is encoded again next time; nothing is thrown through a C entry
+  }
   return true;
 }
 
