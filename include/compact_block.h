@@ -16,7 +16,8 @@
  * magnitude of its block inside the type's range (at least 2^-127; 1 for a block of zeros).  Scaling a floating-point number by a power of
  * two is exact, so this loses nothing against a 32-bit scale except part of one binade at the bottom of the range,
  * and the tensor cores take such scales as operands.  A block that holds an infinity or a NaN gets the scale byte 255, which is
- * NaN: every product with it is NaN, as it would be with the values themselves.
+ * NaN: every sum that a value of the block enters is NaN.  (With the values themselves an infinity could stay one, and of a 128 x 128 block only
+ * the rows that hold such a value would be touched, not all 128.)
  * Layout of the scales of a matrix of `rows` x `cols`: groups of four column blocks,
  *     byte scales[(g * lds + i) * 4 + j] scales columns 128 (4 g + j) .. 128 (4 g + j) + 127 of row i,
  * g < compact_fp8_scale_groups(cols), lds >= rows.  Bytes of column blocks past the last one are written as 127 (scale 1).

@@ -1,9 +1,10 @@
 // RMS norm with the residual's addition.  Forward: h = x + res, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w, out in the
 // input's type and/or in 8 bits with a scale for each 128 columns.  Backward, with g = dy w:
 // dx = rstd g - h rstd^3 mean(g h) + dres,  dw = sum over tokens of dy h rstd.
-// Both are bound by memory: a row is read once and written once.  (16384 x 4096 bf16: forward with residual and both outputs 102 us,
-// 5.9 TB/s; backward with residual gradient 82 us, 6.5 TB/s.  The 8-bit output alone, without residual, is bound by instruction
-// issue: 55 us for 31 us of traffic.)
+// Both are bound by memory: a row is read once and written once.  (16384 x 4096 bf16, calls in a replayed graph: forward with
+// residual and both outputs 103 us, 5.9 TB/s; y alone 44 us, 6.1; backward with residual gradient 78 us, 6.9, and 82 with the weight's and the sum
+// over CTAs.  The 8-bit output alone, without residual, is bound by instruction issue: 55 us for 31 us of traffic.  fp32, forward with
+// both outputs 206 us, 5.5 TB/s.)
 //
 // LANES threads, a group, share a row.  A thread holds U units of sixteen columns, eight neighbouring lanes a block of 128, whose
 // maximum the 8-bit output needs: three shuffles for sixteen values.  A unit is two vectors of eight: of 16-bit values, columns
@@ -254,7 +255,7 @@ struct NormFwdArgs {
 };
 
 // RES: with a residual (then h is stored too, unless NULL).  OUT: 1 for y, 2 for the 8-bit output, 3 for both, 0 for h alone.  Each is a kernel of its
-// own: tests of NULL pointers inside the loops cost the 16384 x 4096 forward without residual 57 us against 45.
+// own: tests of NULL pointers inside the loops cost the 16384 x 4096 forward without residual 57 us against 44.
 template <typename T, int LANES, int U, bool RES, int OUT>
 __global__ void __launch_bounds__(norm_fwd_threads(sizeof(T), U)) rms_norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];

@@ -17,7 +17,7 @@
 //     loop by the power cap: 16384 x 11008 x 4096 585 us, 2.5 PFLOP/s at 1.13 GHz, 93 % of the tensor pipe's cycles.
 //   product_split_kernel: few rows of A (decoding).  The rows of B are the M operand, so that a tile reads 128 rows of the weight
 //     and the tokens are the N operand (16 to 128); a cluster of up to eight CTAs splits K, and its sums meet in
-//     shared memory in a fixed order.  Bound by reading the weight: one token by 11008 x 4096 11.7 us, 5.8 TB/s after some 4 us of
+//     shared memory in a fixed order.  Bound by reading the weight: one token by 11008 x 4096 11.5 us, 6 TB/s after some 4 us of
 //     start, first load and sums.
 #pragma once
 #include "block_common.cuh"
@@ -777,7 +777,9 @@ inline PairPlan pair_plan(int M, int N, int K) {
   // Narrow tiles spend more time on barriers than on MMAs: two k-steps to each (256 x 4096 x 4096 9.2 us against 10.4).  Wide ones keep the
   // six stages of one, for the loads' sake (16384 x 4096 x 4096 214 us against 216).
   p.per_barrier = p.bn <= 128 ? 2 : 1;
-  // B beyond 48 MB goes through the L2 in panels of column tiles (never narrower than a round of tiles is tall)
+  // B beyond 48 MB goes through the L2 in panels of column tiles (never narrower than a round of tiles is tall).  Rows of A by K -> N, with
+  // panels and without: 16384 by 4096 -> 14336 802 us against 850, 8192 -> 8192 883 against 985, 4096 -> 22016 1215 against 1396, 4096 -> 28672
+  // (three) 1566 against 2008; where A is short they make no difference: 4096 by 4096 -> 14336 206 against 209, 1024 57 against 56.
   p.panel_cols = p.tiles_n;
   const long long b_bytes = (long long)K * N, most = 48ll << 20;
   if (b_bytes > most) {
@@ -836,9 +838,14 @@ inline int resident_clusters(unsigned size) {
   return k;
 }
 
-// Which kernel: the splitting one up to 128 tokens where K can be split (4096 x 4096, 77 tokens: 7.7 us against 10.3 with pairs; 128: 9.0
-// against 10.4; 200: 11.6 against 10.4), up to 64 where the weight has a tile for most SMs already (4096 x 11008, 77 tokens: 16.1
-// against 14.5; one: 11.7 against 20.9).
+// Which kernel: the splitting one up to 128 tokens where K can be split, up to 64 where the weight has a tile for most SMs already.  Times of
+// the splitting kernel and of the pairs, weights coming from memory, in us:
+//     4096 -> 4096     1 token 7.1, 17.1    64 8.2, 10.3     77 8.9, 10.3    128 9.9, 10.4     200 10.7, 10.4
+//     4096 -> 11008    1 token 11.5, 19.5   64 13.2, 13.2    77 14.5, 13.4   128 16.4, 13.7    200 26.8, 14.0
+//     11008 -> 4096    1 token 11.3, 38.8   64 12.7, 22.4    77 13.8, 22.5   128 14.8, 22.7    200 17.5, 22.9
+//     2736 -> 1024     1 token 5.3, 10.4    64 6.6, 7.2      77 7.1, 7.3     128 8.6, 7.3      200 7.6, 7.3
+//     512 -> 1376      1 token 3.3, 4.4     64 4.8, 3.8      77 5.2, 3.8     128 6.6, 3.9      200 6.2, 3.7
+// The rule looks at neither a short K, where the pairs would win from 32 tokens on, nor a long one, where splitting would up to 200.
 inline bool prefer_split(int M, int N) { return M <= 64 || (M <= 128 && (N + 127) / 128 <= NUM_SMS / 2); }
 
 inline compact_status_t product_split(const ProductCall& c) {

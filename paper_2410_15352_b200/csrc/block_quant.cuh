@@ -12,7 +12,8 @@ constexpr int QR_THREADS = QR_ROWS * 16;
 
 // A half warp takes the four column blocks of one row whose scales make up one 32-bit word: its four loads are
 // independent, and it writes the word whole.  Neighbouring CTAs take neighbouring groups of the same eight rows.  What is read
-// once is marked so.  (16384 x 4096 bf16: 34.4 us, 5.9 TB/s; sixteen rows and 48 registers a thread 36.0.)
+// once is marked so.  (16384 x 4096 bf16, calls in a replayed graph: 34.7 us, 5.8 TB/s; sixteen rows and 48 registers a thread 36.6.
+// fp32 51.2, 6.6 TB/s.)
 template <typename T, int FP8>
 __global__ void __launch_bounds__(QR_THREADS, sizeof(T) == 2 ? 12 : 8) quantize_rows_kernel(const T* X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* Q,
                                                                                                        int64_t ldq, uint32_t* scales, int64_t lds, int groups) {
@@ -46,8 +47,8 @@ __global__ void __launch_bounds__(QR_THREADS, sizeof(T) == 2 ? 12 : 8) quantize_
 
 // A CTA takes one 128 x 128 block.  Its half warps hold four neighbouring rows each, twice (rows 4 h .. 4 h + 3 and
 // 64 further), so that a lane's four rows of one column make one word of the transpose; the words go through shared
-// memory (pitch 33 words) and leave as 16-byte pieces of the transpose's rows.  (4096 x 11008 bf16: 32.3 us, 5.6 TB/s; with two
-// CTAs of 112 registers a thread to an SM instead of four 43.9.)
+// memory (pitch 33 words) and leave as 16-byte pieces of the transpose's rows.  (4096 x 11008 bf16, calls in a replayed graph: 32.6 us, 5.5 TB/s;
+// with two CTAs of 112 registers a thread to an SM instead of four 42.5.  fp32, two CTAs: 48.7, 5.6 TB/s.)
 constexpr int QT_THREADS = 256;
 constexpr int QT_CTAS = 4;         // of bf16 blocks: 64 registers a thread
 template <typename T, int FP8>

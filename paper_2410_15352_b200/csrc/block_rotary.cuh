@@ -83,7 +83,8 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS) rotary_kernel(const __g
   }
   __syncthreads();
   // One piece at a time to a thread: with 2048 threads to an SM that keeps 64 KB on their way, and leaves registers for all of them.
-  // (16384 tokens of 64 heads of 128, bf16: 81 us; two pieces, half the threads 96; four, a quarter, 131.)
+  // (16384 tokens of 64 heads of 128, bf16, calls in a replayed graph: 85 us, 6.3 TB/s; fp32 163, 6.6 TB/s.  Two pieces, half the threads, took a
+  // fifth longer; four, a quarter, 1.6 times as long.)
   const uint32_t items = (uint32_t)(nt * nh * a.pieces);
   for (uint32_t i = threadIdx.x; i < items; i += ROT_THREADS) {
     const uint32_t th = quotient(i, a.pieces_magic);
